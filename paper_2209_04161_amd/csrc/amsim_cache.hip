@@ -677,7 +677,7 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
     int pid[2];
     const int8_t *kp[2], *vp[2];
     float ks[2], vs[2];
-    bool bad[2];  // a scale that is no number
+    bool seen[2], bad[2];  // by a row of the tile of rows at all; a scale that is no number
     auto load_numbers = [&](int t0) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -696,6 +696,7 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
             vp[h] = a.v + from + slot;
             vs[h] = load_vector(a.vs + at);
             ks[h] = load_vector(a.ks + at);
+            seen[h] = t0 + 32 * h < range.end && t0 + 32 * h + 32 > range.begin;
             bad[h] = !ok;
         }
     };
@@ -734,14 +735,15 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
         }
     };
     // the value scales relative to R, the power of two above the largest so far (so that another R changes no
-    // rounding): what P takes (2^-20 at least) and the power of two that the integers take
+    // rounding): what P takes (2^-20 at least) and the power of two that the integers take.  A page past the keys or
+    // before the window, which shares a tile with one that is seen, may hold any scale: it counts as zeros.
     float big = 0.0f, inv_big = 0.0f, held = 0.0f, fold[2], rest[2], ksc[2];
     bool bad_now[2];
     auto take_scales = [&] {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            bad[h] = bad[h] || !(ks[h] < __builtin_inff()) || !(vs[h] < __builtin_inff());
-            if (bad[h]) ks[h] = vs[h] = 0.0f;
+            bad[h] = seen[h] && (bad[h] || !(ks[h] < __builtin_inff()) || !(vs[h] < __builtin_inff()));
+            if (bad[h] || !seen[h]) ks[h] = vs[h] = 0.0f;
         }
         const float most = __builtin_fmaxf(vs[0], vs[1]);
         if (most > big) {
