@@ -3,6 +3,8 @@
 //
 // Layout: keys [page][head][token][d], values [page][head][d][token] (each page's values transposed, so
 // that the lanes of the second product read runs of tokens), scales [page][head].
+#include <type_traits>
+
 #include "amsim_q8.h"
 
 namespace {
@@ -578,6 +580,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 && DT <= 128 ? 3 : 2) void a
     }
 }
 
+// 2^e, or 0 below an FP32 number's range.
+__device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, e > -127 ? uint32_t(e + 127) << 23 : 0u); }
+
 // Places in LDS of the c-th 16 bytes of row r of a K tile (rows of DT FP16) and of a V^T tile (rows of 64).  The
 // 16 lanes that read one c of 16 rows get 16 different places modulo the 256 bytes of the banks, and each 8 of
 // them 8 different ones modulo 128.
@@ -602,10 +607,10 @@ __device__ __forceinline__ int k_place(int r, int c)
 //
 // 32 x 32 tiles: S^T of 32 tokens and 32 rows leaves a lane 16 scores of one row, the rows of K in LDS in such an
 // order that they are two runs of 8 tokens, the operand of O^T = V^T P^T.  The scale of a page's values
-// goes into P, relative to R, set by the largest one so far (uniform; O is held in units of it); below 2^-20
-// of R the rest of it goes into the integers as they are converted.
+// goes into P, relative to R, set by the largest one so far (uniform; O is held in units of it), until scales lie
+// too far apart for that.
 template <typename T, int DT, int TEAMS>
-__global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_kernel(AttnArgs a)
+__global__ __launch_bounds__(256 * TEAMS, DT > 128 ? 1 : DT <= 64 && TEAMS == 1 && sizeof(T) == 2 ? 3 : 2) void attend_tiles_kernel(AttnArgs a)
 {
     constexpr int WAVES = 4, STRIDE = 64 * TEAMS;
     constexpr int TERMS = sizeof(T) == 4 ? 2 : 1;
@@ -670,34 +675,40 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
         }
     }
 
-    const int mask = a.s.page - 1, page_bytes = a.s.page * a.d;
+    // the sequence's row of the page table, and the head's places in the cache (few scalar registers, of which the loop
+    // below takes nearly all)
+    const int mask = a.s.page - 1, page_bytes = a.s.page * a.d, blocks = int(a.s.ld_table);
+    const int *const table = a.s.table + b * a.s.ld_table;
+    const int8_t *const keys = a.k + int64_t(head) * page_bytes, *const values = a.v + int64_t(head) * page_bytes;
+    const float *const key_scales = a.ks + head, *const value_scales = a.vs + head;
+    const uint32_t page_stride = uint32_t(a.heads) * uint32_t(page_bytes);  // below 2^32: 65535 heads of 256 x 256
     i32x4 kw[PER], vw[PER];
     // of the tile from t0 on: the numbers of its halves' pages (read a tile before the rest, which waits for
     // them), where its keys and values begin, and their scales
     int pid[2];
     const int8_t *kp[2], *vp[2];
     float ks[2], vs[2];
-    bool seen[2], bad[2];  // by a row of the tile of rows at all; a scale that is no number
+    int bad;  // bit h: the page has no place in the cache
     auto load_numbers = [&](int t0) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int blk = (t0 + 32 * h) >> a.s.shift;
-            pid[h] = load_vector(a.s.table + b * a.s.ld_table + (blk < a.s.ld_table ? blk : 0));
+            pid[h] = load_vector(table + (blk < blocks ? blk : 0));
         }
     };
     auto load_pages = [&](int t0) {
+        bad = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int n = __builtin_amdgcn_readfirstlane(pid[h]);
             const bool ok = n >= 0 && n < a.s.n_pages;
-            const int64_t at = int64_t(ok ? n : 0) * a.heads + head, from = at * page_bytes;
+            const uint64_t at = uint64_t(ok ? n : 0) * uint32_t(a.heads), from = uint64_t(ok ? n : 0) * page_stride;
             const int slot = (t0 + 32 * h) & mask;
-            kp[h] = a.k + from + slot * a.d;
-            vp[h] = a.v + from + slot;
-            vs[h] = load_vector(a.vs + at);
-            ks[h] = load_vector(a.ks + at);
-            seen[h] = t0 + 32 * h < range.end && t0 + 32 * h + 32 > range.begin;
-            bad[h] = !ok;
+            kp[h] = keys + from + slot * a.d;
+            vp[h] = values + from + slot;
+            vs[h] = load_vector(value_scales + at);
+            ks[h] = load_vector(key_scales + at);
+            bad |= ok ? 0 : 1 << h;
         }
     };
     // a thread's pieces: token tok of the keys, 16 elements from c * 16 on; row dd of the values, 16 tokens from g * 16
@@ -720,8 +731,8 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
     };
     // pieces of 16 bytes to two of eight FP16 values; their place in a row is turned by the row's number, so that
     // the reads of sixteen rows at one place spread over the banks
-    auto store_tile = [&](char *buf, const float (&rest)[2]) {
-        const _Float16 f = _Float16(vg < 2 ? rest[0] : rest[1]);
+    auto store_tile = [&](char *buf, const float (&factor)[2]) {
+        const _Float16 f = _Float16((vg < 2 ? factor[0] : factor[1]) > 0.0f ? 1.0f : 0.0f);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int tok = (i * 64 * WAVES + tid) / (DT / 16), dd = (i * 64 * WAVES + tid) / 4;
@@ -734,33 +745,41 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
             }
         }
     };
-    // the value scales relative to R, the power of two above the largest so far (so that another R changes no
-    // rounding): what P takes (2^-20 at least) and the power of two that the integers take.  A page past the keys or
-    // before the window, which shares a tile with one that is seen, may hold any scale: it counts as zeros.
-    float big = 0.0f, inv_big = 0.0f, held = 0.0f, fold[2], rest[2], ksc[2];
-    bool bad_now[2];
-    auto take_scales = [&] {
+    // The value scales relative to R, the power of two above the largest so far (so that another R changes no
+    // rounding): what P takes.  That holds scales within 2^14 of each other.  From the first tile with others on
+    // (`spread`) each page's sums are multiplied by its scale in FP32, as for few rows, and R is 2^14, which makes O the
+    // numerator itself: a scale however large or small takes nothing from rows that do not see its page.  A page past
+    // the keys or before the window, which shares a tile with one that is seen, counts as zeros.
+    // (All of it uniform, in scalar registers: R and O's unit as exponents, 126 for 1 and 0 for none yet.)
+    constexpr int FAR = 14;
+    int big = 0, held = 0;
+    float fold[2], ksc[2];
+    int bad_now, spread = 0;
+    auto take_scales = [&](int t0) {
+        uint32_t vb[2], kb[2];
+        bad_now = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            bad[h] = seen[h] && (bad[h] || !(ks[h] < __builtin_inff()) || !(vs[h] < __builtin_inff()));
-            if (bad[h] || !seen[h]) ks[h] = vs[h] = 0.0f;
+            vb[h] = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, vs[h]));
+            kb[h] = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, ks[h]));
+            const int seen = t0 + 32 * h < range.end && t0 + 32 * h + 32 > range.begin ? 1 : 0;
+            const int wrong = bad >> h & 1 || vb[h] >= 0x7F800000u || kb[h] >= 0x7F800000u ? 1 : 0;
+            if (wrong || !seen) vb[h] = kb[h] = 0;
+            bad_now |= (wrong & seen) << h;
+            ksc[h] = __builtin_bit_cast(float, kb[h]);
         }
-        const float most = __builtin_fmaxf(vs[0], vs[1]);
-        if (most > big) {
-            int e = __builtin_amdgcn_frexp_expf(most);
-            e = e < 126 ? e : 126;
-            big = __builtin_ldexpf(1.0f, e);
-            inv_big = __builtin_ldexpf(1.0f, -e);
+        const int e0 = vb[0] >> 23, e1 = vb[1] >> 23, most = e0 > e1 ? e0 : e1;
+        if (!spread) {
+            const bool far = big > 0 && most > big + FAR;
+            big = most > big ? most : big;
+            spread = far || (e0 > 0 && e0 < big - FAR) || (e1 > 0 && e1 < big - FAR) ? 1 : 0;
+            if (spread) big = 126 + FAR;
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float c = vs[h] * inv_big;
-            const int e = __builtin_amdgcn_frexp_expf(c);  // c < 2^-20: e <= -20
-            const bool tiny = c < 0x1p-20f;
-            fold[h] = !tiny ? c : c > 0.0f ? __builtin_ldexpf(c, -20 - e) : 0x1p-20f;
-            rest[h] = !tiny ? 1.0f : c > 0.0f ? __builtin_ldexpf(1.0f, e + 20) : 0.0f;
-            ksc[h] = ks[h];
-            bad_now[h] = bad[h];
+            const int e = int(vb[h] >> 23);  // 0: a scale of zero
+            const int at = 126 + e - big;
+            fold[h] = __builtin_bit_cast(float, e > 0 && at > 0 ? (vb[h] & 0x7FFFFFu) | uint32_t(at) << 23 : 0u);
         }
     };
 
@@ -772,10 +791,11 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
         load_pages(t0);
         load_tile();
         load_numbers(t0 + STRIDE);
-        take_scales();
-        store_tile(mem, rest);
+        take_scales(t0);
+        store_tile(mem, fold);
     }
-    for (int turn = begin; turn < end; turn += STRIDE, t0 += STRIDE, buf ^= DT * 256) {  // as many turns for each team
+    auto take_turn = [&](auto with_spread) {
+        constexpr bool SPREAD = decltype(with_spread)::value;
         const bool more = t0 + STRIDE < end;
         if (more) {
             load_pages(t0 + STRIDE);
@@ -809,12 +829,12 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
                         if (!(key <= last && key >= first)) sc[h][r] = -__builtin_inff();
                     }
             }
-            if (__builtin_expect(bad_now[0] || bad_now[1], 0)) {  // reaches the rows that see the page
+            if (__builtin_expect(bad_now, 0)) {  // reaches the rows that see the page
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (bad_now[h] && sc[h][r] != -__builtin_inff()) sc[h][r] = __builtin_nanf("");
+                        if ((bad_now >> h & 1) && sc[h][r] != -__builtin_inff()) sc[h][r] = __builtin_nanf("");
             }
             float top = m, f[2];
 #pragma unroll
@@ -831,7 +851,7 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
                 keep_branch();
                 float alpha = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
                 l *= alpha;
-                alpha *= held * inv_big;
+                alpha *= power(held > 0 ? held - big : -127);
                 held = big;
 #pragma unroll
                 for (int dt = 0; dt < DTILES; ++dt) o[dt] *= alpha;
@@ -842,14 +862,15 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 // the value scale as part of the exponent, or for FP32 (whose P keeps 22 bits) as a factor
-                const float from = TERMS == 1 ? base - __builtin_amdgcn_logf(fold[h]) : base;
+                const float c = SPREAD ? 1.0f : fold[h] > 0.0f ? fold[h] : 0x1p-20f;
+                const float from = TERMS == 1 && !SPREAD ? base - __builtin_amdgcn_logf(c) : base;
                 float sum = 0.0f;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h][r], f[h], -from));
                     if constexpr (TERMS == 2) {
                         sum += p;
-                        p *= fold[h];
+                        p *= c;
                     }
                     _Float16 hi, lo;
                     split_f16(p, hi, lo);
@@ -863,28 +884,55 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
                         sum = __builtin_amdgcn_fdot2(f16x2{pf[0][h * 2 + r / 8][r % 8], pf[0][h * 2 + r / 8][r % 8 + 1]}, ones,
                                                      sum, false);
                 }
-                l = __builtin_fmaf(sum, TERMS == 1 ? __builtin_amdgcn_rcpf(fold[h]) : 1.0f, l);
+                l = __builtin_fmaf(sum, TERMS == 1 && !SPREAD ? __builtin_amdgcn_rcpf(c) : 1.0f, l);
             }
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
+            if constexpr (SPREAD) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int dt = 0; dt < DTILES; ++dt) {
-                    const f16x8 vf = *reinterpret_cast<const f16x8 *>(vb + v_place(dt * 32 + col, k * 2 + half));
+                    for (int dt = 0; dt < DTILES; ++dt) {
+                        f32x16 part = {};
 #pragma unroll
-                    for (int term = 0; term < TERMS; ++term)
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[term][k], o[dt], 0, 0, 0);
-                }
-            read_ahead<4 * DTILES, TERMS>();
+                        for (int k = h * 2; k < h * 2 + 2; ++k) {
+                            const f16x8 vf = *reinterpret_cast<const f16x8 *>(vb + v_place(dt * 32 + col, k * 2 + half));
+#pragma unroll
+                            for (int term = 0; term < TERMS; ++term)
+                                part = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[term][k], part, 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[dt][r] = __builtin_fmaf(part[r], fold[h], o[dt][r]);
+                        __builtin_amdgcn_sched_barrier(0);  // one `part` at a time
+                    }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int dt = 0; dt < DTILES; ++dt) {
+                        const f16x8 vf = *reinterpret_cast<const f16x8 *>(vb + v_place(dt * 32 + col, k * 2 + half));
+#pragma unroll
+                        for (int term = 0; term < TERMS; ++term)
+                            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[term][k], o[dt], 0, 0, 0);
+                    }
+                read_ahead<4 * DTILES, TERMS>();
+            }
             __builtin_amdgcn_s_setprio(0);
         }
         if (more) {
-            take_scales();
-            store_tile(mem + (buf ^ DT * 256), rest);
+            take_scales(t0 + STRIDE);
+            store_tile(mem + (buf ^ DT * 256), fold);
         }
-    }
-    l += __shfl_xor(l, 32);
+        t0 += STRIDE;
+        buf ^= DT * 256;
+    };
+    int turn = begin;  // as many turns for each team
+    for (; turn < end && !spread; turn += STRIDE) take_turn(std::false_type());
+    for (; turn < end; turn += STRIDE) take_turn(std::true_type());
+    // P was 2^14 for m, O in units of `held`: their true values from here on, since another team's (or chunk's) unit may
+    // be any other
+    l = (l + __shfl_xor(l, 32)) * 0x1p-14f;
+    float f = power(held > 0 ? held - 126 - 14 : -127);
     if constexpr (TEAMS == 2) {  // the second team's sums, through LDS, to the first team's
         f32x4 *const so = reinterpret_cast<f32x4 *>(smem);
         float *const sm = reinterpret_cast<float *>(smem + DT * 512);
@@ -894,28 +942,28 @@ __global__ __launch_bounds__(256 * TEAMS, DT <= 128 ? 2 : 1) void attend_tiles_k
             for (int dt = 0; dt < DTILES; ++dt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    so[(dt * 4 + r) * 256 + tid] = f32x4{o[dt][r * 4], o[dt][r * 4 + 1], o[dt][r * 4 + 2], o[dt][r * 4 + 3]};
+                    so[(dt * 4 + r) * 256 + tid] =
+                        f32x4{o[dt][r * 4], o[dt][r * 4 + 1], o[dt][r * 4 + 2], o[dt][r * 4 + 3]} * f;
             sm[tid] = m;
             sm[256 + tid] = l;
-            sm[512 + tid] = held;
         }
         __syncthreads();
         if (team == 1) return;
-        const float m1 = sm[tid], held1 = sm[512 + tid], top = __builtin_fmaxf(m, m1), most = __builtin_fmaxf(held, held1);
+        const float m1 = sm[tid], top = __builtin_fmaxf(m, m1);
         const float w0 = m > -__builtin_inff() ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
         const float w1 = m1 > -__builtin_inff() ? __builtin_amdgcn_exp2f(m1 - top) : 0.0f;
-        const float f0 = most > 0.0f ? w0 * (held / most) : 0.0f, f1 = most > 0.0f ? w1 * (held1 / most) : 0.0f;
         l = l * w0 + sm[256 + tid] * w1;
+        const float f0 = f * w0;
 #pragma unroll
         for (int dt = 0; dt < DTILES; ++dt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[dt][r] = __builtin_fmaf(o[dt][r], f0, so[(dt * 4 + r / 4) * 256 + tid][r % 4] * f1);
+            for (int r = 0; r < 16; ++r) o[dt][r] = __builtin_fmaf(o[dt][r], f0, so[(dt * 4 + r / 4) * 256 + tid][r % 4] * w1);
         m = top;
-        held = most;
+        f = 1.0f;
     }
     if (!live) return;
     const bool one = a.splits == 1;
-    const float f = (one ? (l != 0.0f ? 1.0f / l : 0.0f) : 1.0f) * held;
+    if (one) f *= l != 0.0f ? 1.0f / l : 0.0f;
     const int64_t unit = (int64_t(s.start) + tq) * a.q_heads + hq;
     float *part = a.part + (unit * a.splits + split) * a.d;
     if (!one && half == 0) {
