@@ -607,8 +607,8 @@ __device__ __forceinline__ int k_place(int r, int c)
 //
 // 32 x 32 tiles: S^T of 32 tokens and 32 rows leaves a lane 16 scores of one row, the rows of K in LDS in such an
 // order that they are two runs of 8 tokens, the operand of O^T = V^T P^T.  The scale of a page's values
-// goes into P, relative to R, set by the largest one so far (uniform; O is held in units of it), until scales lie
-// too far apart for that.
+// goes into P and the integers, relative to R, set by the largest one so far (uniform; O is held in units of it), until
+// scales lie too far apart for that.
 template <typename T, int DT, int TEAMS>
 __global__ __launch_bounds__(256 * TEAMS, DT > 128 ? 1 : DT <= 64 && TEAMS == 1 && sizeof(T) == 2 ? 3 : 2) void attend_tiles_kernel(AttnArgs a)
 {
@@ -731,8 +731,8 @@ __global__ __launch_bounds__(256 * TEAMS, DT > 128 ? 1 : DT <= 64 && TEAMS == 1 
     };
     // pieces of 16 bytes to two of eight FP16 values; their place in a row is turned by the row's number, so that
     // the reads of sixteen rows at one place spread over the banks
-    auto store_tile = [&](char *buf, const float (&factor)[2]) {
-        const _Float16 f = _Float16((vg < 2 ? factor[0] : factor[1]) > 0.0f ? 1.0f : 0.0f);
+    auto store_tile = [&](char *buf, const uint32_t (&rest)[2]) {
+        const f16x2 f = __builtin_bit_cast(f16x2, vg < 2 ? rest[0] : rest[1]);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int tok = (i * 64 * WAVES + tid) / (DT / 16), dd = (i * 64 * WAVES + tid) / 4;
@@ -741,19 +741,21 @@ __global__ __launch_bounds__(256 * TEAMS, DT > 128 ? 1 : DT <= 64 && TEAMS == 1 
             for (int u = 0; u < 2; ++u) {
                 *reinterpret_cast<f16x8 *>(buf + k_place<DT>(r, kc * 2 + u)) = bytes_to_f16(kw[i][2 * u], kw[i][2 * u + 1]);
                 *reinterpret_cast<f16x8 *>(buf + 64 * DT * 2 + v_place(dd, vg * 2 + u)) =
-                    bytes_to_f16(vw[i][2 * u], vw[i][2 * u + 1], f16x2{f, f});
+                    bytes_to_f16(vw[i][2 * u], vw[i][2 * u + 1], f);
             }
         }
     };
-    // The value scales relative to R, the power of two above the largest so far (so that another R changes no
-    // rounding): what P takes.  That holds scales within 2^14 of each other.  From the first tile with others on
-    // (`spread`) each page's sums are multiplied by its scale in FP32, as for few rows, and R is 2^14, which makes O the
-    // numerator itself: a scale however large or small takes nothing from rows that do not see its page.  A page past
-    // the keys or before the window, which shares a tile with one that is seen, counts as zeros.
+    // A page's value scale is f 2^e, 0.5 <= f < 1.  P takes f (all its bits stay: rows whose weight lies in many faint
+    // keys keep it, and so does the sum of the rounded P), the integers take 2^e relative to R, the power of two above
+    // the largest scale so far, exactly: down to 2^-14 a normal FP16 number.  From the first tile with scales
+    // further apart on (`spread`) each page's sums are multiplied by its scale in FP32, as for few rows, and R is 2^14,
+    // which makes O the numerator itself: a scale however large or small takes nothing from rows that do not
+    // see its page.  A page past the keys or before the window, which shares a tile with one that is seen, counts as zeros.
     // (All of it uniform, in scalar registers: R and O's unit as exponents, 126 for 1 and 0 for none yet.)
     constexpr int FAR = 14;
     int big = 0, held = 0;
     float fold[2], ksc[2];
+    uint32_t rest[2];  // 2^e / R, twice, as FP16
     int bad_now, spread = 0;
     auto take_scales = [&](int t0) {
         uint32_t vb[2], kb[2];
@@ -778,8 +780,15 @@ __global__ __launch_bounds__(256 * TEAMS, DT > 128 ? 1 : DT <= 64 && TEAMS == 1 
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int e = int(vb[h] >> 23);  // 0: a scale of zero
+            const uint32_t mantissa = vb[h] & 0x7FFFFFu;
             const int at = 126 + e - big;
-            fold[h] = __builtin_bit_cast(float, e > 0 && at > 0 ? (vb[h] & 0x7FFFFFu) | uint32_t(at) << 23 : 0u);
+            if (spread) {
+                fold[h] = __builtin_bit_cast(float, e > 0 && at > 0 ? mantissa | uint32_t(at) << 23 : 0u);
+                rest[h] = 0x3C003C00u;
+            } else {
+                fold[h] = __builtin_bit_cast(float, mantissa | 126u << 23);
+                rest[h] = e > 0 ? uint32_t(15 + e - big) * 0x04000400u : 0u;
+            }
         }
     };
 
@@ -792,7 +801,7 @@ __global__ __launch_bounds__(256 * TEAMS, DT > 128 ? 1 : DT <= 64 && TEAMS == 1 
         load_tile();
         load_numbers(t0 + STRIDE);
         take_scales(t0);
-        store_tile(mem, fold);
+        store_tile(mem, rest);
     }
     auto take_turn = [&](auto with_spread) {
         constexpr bool SPREAD = decltype(with_spread)::value;
@@ -862,7 +871,7 @@ __global__ __launch_bounds__(256 * TEAMS, DT > 128 ? 1 : DT <= 64 && TEAMS == 1 
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 // the value scale as part of the exponent, or for FP32 (whose P keeps 22 bits) as a factor
-                const float c = SPREAD ? 1.0f : fold[h] > 0.0f ? fold[h] : 0x1p-20f;
+                const float c = SPREAD ? 1.0f : fold[h];
                 const float from = TERMS == 1 && !SPREAD ? base - __builtin_amdgcn_logf(c) : base;
                 float sum = 0.0f;
 #pragma unroll
@@ -921,7 +930,7 @@ __global__ __launch_bounds__(256 * TEAMS, DT > 128 ? 1 : DT <= 64 && TEAMS == 1 
         }
         if (more) {
             take_scales(t0 + STRIDE);
-            store_tile(mem + (buf ^ DT * 256), fold);
+            store_tile(mem + (buf ^ DT * 256), rest);
         }
         t0 += STRIDE;
         buf ^= DT * 256;
