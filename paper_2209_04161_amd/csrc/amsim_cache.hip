@@ -509,12 +509,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 && DT <= 128 ? 3 : 2) void a
                 pf[0][t / 2][t % 2 * 4 + r] = hi;
                 if constexpr (TERMS == 2) pf[1][t / 2][t % 2 * 4 + r] = lo;
             }
-        // a page that a row sees nothing of adds nothing to it, whatever its scale
+        // a page that a row sees nothing of adds nothing to it, whatever its scale; P is 2^14 for m, which O need not
+        // have the range for
         float f[Pages<WHOLE>::N];
 #pragma unroll
         for (int h = 0; h < Pages<WHOLE>::N; ++h) {
             const int from = t0 + 32 * h, to = from + (WHOLE ? 64 : 32);
-            f[h] = last >= from && first < to ? pg.vs[h] : 0.0f;
+            f[h] = last >= from && first < to ? pg.vs[h] * 0x1p-14f : 0.0f;
         }
 #pragma unroll
         for (int dt = 0; dt < DTILES; ++dt) {
@@ -535,6 +536,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 && DT <= 128 ? 3 : 2) void a
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+    l *= 0x1p-14f;
 
     // the waves' sums, at the largest maximum of the row
     if (grp == 0) lm[wave][row16] = m;
