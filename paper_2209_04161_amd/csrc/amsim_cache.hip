@@ -51,6 +51,7 @@ struct AppendArgs {
     int8_t *pool[2];
     float *scale[2];
     int heads, d, touched;
+    unsigned first;  // the launch's first workgroup
 };
 
 // One workgroup to a page that gets new tokens, a head, and keys or values: the new tokens' largest
@@ -63,7 +64,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
     __shared__ float lds[4];
-    unsigned id = blockIdx.x;
+    unsigned id = blockIdx.x + a.first;
     const int which = id & 1;
     id >>= 1;
     const int head = id % a.heads;
@@ -198,6 +199,7 @@ struct AttnArgs {
     int64_t units;      // new tokens x query heads
     int splits, chunk;  // a sequence's keys in chunks of `chunk` tokens, `splits` of them at most for any row
     float scale;        // of the scores, with log2(e)
+    unsigned first;     // the launch's first workgroup
 };
 
 // Four 8-bit integers as FP16, exactly: 0x6400 | u is 1024 + u for a byte u, here the integer + 128.
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 && DT <= 128 ? 3 : 2) void a
     __shared__ f32x4 lo[WAVES - 1][DTILES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row16 = lane % 16, grp = lane / 16;
-    unsigned id = blockIdx.x;
+    unsigned id = blockIdx.x + a.first;
     const int split = id % a.splits;
     id /= a.splits;
     const int tile = id % a.tiles;
@@ -624,7 +626,7 @@ __global__ __launch_bounds__(256 * TEAMS, DT > 128 ? 1 : DT <= 64 && TEAMS == 1 
     const int team = TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
     char *const mem = smem + team * (DT * 512);
     const int col = lane & 31, half = lane >> 5;
-    unsigned id = blockIdx.x;
+    unsigned id = blockIdx.x + a.first;
     const int head = id % a.heads;
     id /= a.heads;
     const int split = id % a.splits;
@@ -1247,8 +1249,10 @@ int amsim_cache_append(const amsim_cache8 *cache, int64_t batch, const int32_t *
     if (2 * batch * a.heads >= lim || 2 * batch * a.heads * a.touched >= lim) return AMSIM_ERR_UNSUPPORTED;
     const int64_t groups = 2 * batch * a.heads * a.touched;
     return with_type(dtype, [&](auto t) {
-        hipLaunchKernelGGL((append_kernel<decltype(t)>), dim3(static_cast<unsigned>(groups)), dim3(256), 0,
-                           static_cast<hipStream_t>(stream), a);
+        in_launches(groups, [&](int64_t first, unsigned count) {
+            a.first = unsigned(first);
+            hipLaunchKernelGGL((append_kernel<decltype(t)>), dim3(count), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+        });
         return launch_status();
     });
 }
@@ -1306,12 +1310,15 @@ int amsim_cache_attention(const amsim_cache8 *cache, int64_t batch, const int32_
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
         const hipStream_t st = static_cast<hipStream_t>(stream);
-        if (p.span == 16) {
-            launch_rows<T>(a, p.wide, static_cast<unsigned>(groups), st);
-        } else {
-            const int done = launch_tiles<T>(a, p.wide, static_cast<unsigned>(groups), st);
-            if (done != AMSIM_OK) return done;
-        }
+        int done = AMSIM_OK;
+        in_launches(groups, [&](int64_t first, unsigned count) {
+            a.first = unsigned(first);
+            if (p.span == 16)
+                launch_rows<T>(a, p.wide, count, st);
+            else if (done == AMSIM_OK)
+                done = launch_tiles<T>(a, p.wide, count, st);
+        });
+        if (done != AMSIM_OK) return done;
         if (joins > 0 && p.splits <= kFewSplits)
             hipLaunchKernelGGL((combine_few_kernel<T>), dim3(static_cast<unsigned>(ceil_div(joins, 4))), dim3(256), 0, st,
                                a, p.span, joins);

@@ -138,7 +138,7 @@ __global__ __launch_bounds__(1024) void quantize_long_kernel(FwdArgs a)
 }
 
 template <typename T, bool NORM>
-int launch_fwd(const FwdArgs &a, hipStream_t st)
+void launch_rows(const FwdArgs &a, hipStream_t st)
 {
     const dim3 one(static_cast<unsigned>(a.rows)), four(static_cast<unsigned>(ceil_div(a.rows, 4)));
 #define FWD(THREADS, CH) \
@@ -163,6 +163,21 @@ int launch_fwd(const FwdArgs &a, hipStream_t st)
     else
         hipLaunchKernelGGL((quantize_long_kernel<T>), one, dim3(1024), 0, st, a);
 #undef FWD
+}
+
+template <typename T, bool NORM>
+int launch_fwd(const FwdArgs &a, hipStream_t st)
+{
+    in_launches(a.rows, [&](int64_t first, unsigned count) {
+        FwdArgs p = a;
+        const auto from = [&](const void *t, int64_t ld) { return t ? static_cast<const T *>(t) + first * ld : nullptr; };
+        const auto to = [&](void *t, int64_t ld) { return t ? static_cast<T *>(t) + first * ld : nullptr; };
+        p.x = from(a.x, a.ldx), p.r = from(a.r, a.ldr), p.h = to(a.h, a.ldh), p.y = to(a.y, a.ldy);
+        if (a.q) p.q = a.q + first * a.ldq, p.scale = a.scale + first;
+        if (a.rstd) p.rstd = a.rstd + first;
+        p.rows = count;
+        launch_rows<T, NORM>(p, st);
+    });
     return launch_status();
 }
 

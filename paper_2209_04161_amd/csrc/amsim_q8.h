@@ -32,6 +32,14 @@ inline int with_type(int dtype, F &&f)
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// A launch takes fewer than 2^32 threads: calls f(first, count) for runs of the workgroups (of up to 1024 threads).
+template <typename F>
+inline void in_launches(int64_t groups, F &&f)
+{
+    constexpr int64_t kMost = int64_t(1) << 21;
+    for (int64_t first = 0; first < groups; first += kMost) f(first, unsigned(groups - first < kMost ? groups - first : kMost));
+}
+
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
