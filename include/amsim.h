@@ -299,7 +299,9 @@ int amsim_quantize_rows(int dtype, int64_t rows, int64_t n, const void *x, int64
 /* amsim_gemm_i8: C[i][j] = (sum_k a[i][k] * b[j][k]) * a_scale[i] * b_scale[j] + bias[j], a m x k and b n x k
  * (both with k along the rows: a dense layer's weights stored [out][in]), bias NULL or n floats, C m x n
  * of out_dtype.  The sum is exact (32-bit integers).  k == 0: C is the bias, or zeros.  k < 2^17 and m, n
- * < 2^21, else AMSIM_ERR_UNSUPPORTED.  Device workspace of the size that the query reports (NULL when 0). */
+ * < 2^21, else AMSIM_ERR_UNSUPPORTED; so are calls that would launch 2^32 threads: operands that are not at multiples
+ * of 16 bytes with 2^36 results or more, or, k no multiple of 16, with 2^36 bytes.  Device workspace of the
+ * size that the query reports (NULL when 0). */
 int amsim_gemm_i8_workspace_size(int64_t m, int64_t n, int64_t k, size_t *bytes);
 int amsim_gemm_i8(int64_t m, int64_t n, int64_t k, const int8_t *a, int64_t lda, const float *a_scale,
                   const int8_t *b, int64_t ldb, const float *b_scale, const float *bias, int out_dtype, void *c,

@@ -557,6 +557,11 @@ int amsim_gemm_i8(int64_t m, int64_t n, int64_t k, const int8_t *a, int64_t lda,
     const auto whole = [](const void *p, int64_t ld) { return ((uintptr_t(p) | uintptr_t(ld)) & 15) == 0 && ld < (1 << 23); };
     bool aligned = whole(a, lda) && whole(b, ldb);
     const GemmPlan p = plan_gemm(m, n, k, aligned);
+    // a launch takes fewer than 2^32 threads (small tiles of 137 GB of results, copies of 64 GB of operands do not fit;
+    // larger tiles reach it with results that no memory holds)
+    const int64_t threads = int64_t(p.tiles_m) * p.tiles_n * p.splits * (p.kind == kLarge ? 512 : 256);
+    const int64_t pieces = p.pack && !aligned ? (m + n) * ceil_div(k, 16) : 0;
+    if (threads >= int64_t(1) << 32 || pieces >= int64_t(1) << 32) return AMSIM_ERR_UNSUPPORTED;
     GemmArgs g{a, b, a_scale, b_scale, bias, c, static_cast<int *>(workspace), lda, ldb, ldc, int(m), int(n),
                int(k), p.tiles_m, p.tiles_n, p.splits, p.per};
     const hipStream_t st = static_cast<hipStream_t>(stream);
