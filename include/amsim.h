@@ -339,7 +339,7 @@ int amsim_cache_append(const amsim_cache8 *cache, int64_t batch, const int32_t *
 /* amsim_cache_attention: softmax attention of the new tokens' queries over the cache (which holds the new
  * tokens' keys and values already).  q: element (token, head, i) at token * q_token + head * q_head + i, out
  * likewise; q_heads a multiple of cache->heads, query head h reading key head h / (q_heads / heads).  Scores
- * are scale * (q . k).  causal: the token at position p sees the keys 0 .. p, with window > 0 the last
+ * are scale * (q . k), scale finite and below 2^127 (else AMSIM_ERR_INVALID_ARG).  causal: the token at position p sees the keys 0 .. p, with window > 0 the last
  * `window` of them; not causal (window must be 0): every key.  A token that sees no key gets zeros.
  * max_len bounds what is read.  Device workspace of the size that the query reports (NULL when 0). */
 int amsim_cache_attention_workspace_size(const amsim_cache8 *cache, int64_t batch, int64_t q_heads, int64_t total_new,

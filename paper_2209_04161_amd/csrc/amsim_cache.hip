@@ -1288,6 +1288,8 @@ int amsim_cache_attention(const amsim_cache8 *cache, int64_t batch, const int32_
     int rc = amsim_cache_attention_workspace_size(cache, batch, q_heads, total_new, max_new, max_len, window, &need);
     if (rc != AMSIM_OK) return rc;
     if (!valid_type(dtype) || (window > 0 && !causal)) return AMSIM_ERR_INVALID_ARG;
+    scale *= 1.44269504f;
+    if (!(__builtin_fabsf(scale) < __builtin_inff())) return AMSIM_ERR_INVALID_ARG;
     AttnArgs a{};
     rc = check_seqs(cache, batch, page_table, ld_table, lengths, starts, total_new, max_new, max_len, a.s);
     if (rc != AMSIM_OK) return rc;
@@ -1301,7 +1303,7 @@ int amsim_cache_attention(const amsim_cache8 *cache, int64_t batch, const int32_
     a.q_tok = q_token, a.q_head = q_head, a.o_tok = out_token, a.o_head = out_head;
     a.q_heads = int(q_heads), a.heads = cache->heads, a.d = cache->head_dim, a.group = int(q_heads / cache->heads);
     a.causal = causal != 0, a.window = int(window < (int64_t(1) << 30) ? window : 0);
-    a.scale = scale * 1.44269504f;
+    a.scale = scale;
     a.units = total_new * q_heads;
     a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk;
     const int64_t lim = int64_t(1) << 31, groups = batch * a.heads * a.tiles * a.splits;
