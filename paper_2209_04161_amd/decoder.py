@@ -23,6 +23,13 @@ from . import binding, modules
 Batch = collections.namedtuple("Batch", "page_table lengths starts max_new max_len")
 
 
+def split_heads(qkv, heads, kv_heads, head_dim):
+    """(q, k, v), each [tokens, heads, head_dim], views of the projection's rows."""
+    h, g, d = heads, kv_heads, head_dim
+    return (qkv[:, :h * d].unflatten(1, (h, d)), qkv[:, h * d:(h + g) * d].unflatten(1, (g, d)),
+            qkv[:, (h + g) * d:].unflatten(1, (g, d)))
+
+
 class DecoderBlock(torch.nn.Module):
     """Norm, causal attention, norm, feed-forward (ReLU); the residual's addition is part of the norms."""
 
@@ -41,10 +48,7 @@ class DecoderBlock(torch.nn.Module):
         self.down = modules.AMLinear(hidden, width, lut, m_bits)
 
     def split(self, qkv):
-        """(q, k, v), each [tokens, heads, head_dim], views of the projection's rows."""
-        h, g, d = self.heads, self.kv_heads, self.head_dim
-        return (qkv[:, :h * d].unflatten(1, (h, d)), qkv[:, h * d:(h + g) * d].unflatten(1, (g, d)),
-                qkv[:, (h + g) * d:].unflatten(1, (g, d)))
+        return split_heads(qkv, self.heads, self.kv_heads, self.head_dim)
 
     def forward(self, x, residual=None):
         """(the block's output, the residual stream it is to be added to)"""
@@ -131,20 +135,28 @@ class PagedCache8:
                      max([n for _, n in counts] + [0]), max(lengths + [0]))
 
 
+def _frozen(norm):
+    """The norm as it is now, without gradients."""
+    weight = norm.weight.detach().clone()
+    new = modules.RMSNorm(weight.numel(), norm.eps, weight.device)
+    new.weight = torch.nn.Parameter(weight, requires_grad=False)
+    return new
+
+
 class DecoderBlock8(torch.nn.Module):
-    """A DecoderBlock's weights in 8 bits, with a cache in 8 bits."""
+    """A DecoderBlock's weights as they are now in 8 bits, with a cache in 8 bits."""
 
     def __init__(self, block):
         super().__init__()
-        self.heads, self.kv_heads, self.head_dim, self.split = block.heads, block.kv_heads, block.head_dim, block.split
-        self.norm1, self.norm2 = block.norm1, block.norm2
+        self.heads, self.kv_heads, self.head_dim = block.heads, block.kv_heads, block.head_dim
+        self.norm1, self.norm2 = _frozen(block.norm1), _frozen(block.norm2)
         self.qkv, self.out, self.up, self.down = (modules.Linear8(layer.weight, layer.bias)
                                                   for layer in (block.qkv, block.out, block.up, block.down))
 
     def forward(self, x, residual, cache, batch):
         """(the block's output, the residual stream); cache: this layer's Cache8."""
         y, h = self.norm1.quantized(x, residual)
-        q, k, v = self.split(self.qkv(y, x.dtype))
+        q, k, v = split_heads(self.qkv(y, x.dtype), self.heads, self.kv_heads, self.head_dim)
         table, lengths, starts, max_new, max_len = batch
         binding.amsim_cache_append(cache, table, lengths, k, v, starts, max_new)
         o = binding.amsim_cache_attention(cache, table, lengths, q, starts, max_new, max_len)
@@ -153,12 +165,13 @@ class DecoderBlock8(torch.nn.Module):
 
 
 class Decoder8(torch.nn.Module):
-    """A Decoder's weights in 8 bits, for inference."""
+    """A Decoder's weights as they are now in 8 bits, for inference.  Nothing is shared with the Decoder: it can be trained
+    on, or given up."""
 
     def __init__(self, model):
         super().__init__()
         self.blocks = torch.nn.ModuleList([DecoderBlock8(b) for b in model.blocks])
-        self.norm = model.norm
+        self.norm = _frozen(model.norm)
 
     def cache(self, pages, page_tokens=64):
         b = self.blocks[0]

@@ -202,7 +202,7 @@ class Linear8(torch.nn.Module):
         q, scale = binding.amsim_quantize_rows(weight.detach().t().contiguous())
         self.register_buffer("weight", q)          # [out, in]
         self.register_buffer("weight_scale", scale)
-        self.register_buffer("bias", bias.detach().float() if bias is not None else None)
+        self.register_buffer("bias", bias.detach().float().clone() if bias is not None else None)
 
     def forward(self, x, dtype=None):
         """x: a tensor [tokens, in], quantised here, or a pair (q, scale); the result has x's type, or `dtype`."""
