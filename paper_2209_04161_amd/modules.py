@@ -158,6 +158,7 @@ class _RMSNormFn(torch.autograd.Function):
         return (r.y, r.h) if ctx.residual else r.y
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dy, dh=None):
         h, weight, rstd = ctx.saved_tensors
         if dy is None:  # only the sum was used
@@ -169,7 +170,8 @@ class _RMSNormFn(torch.autograd.Function):
 
 
 def rms_norm(x, weight, eps=1e-6, residual=None):
-    """Root-mean-square norm of the rows of x [tokens, n]; with a residual: (norm of the sum, the sum)."""
+    """Root-mean-square norm of the rows of x [tokens, n]; with a residual: (norm of the sum, the sum).  It has first
+    derivatives alone: a backward pass through its gradient raises."""
     return _RMSNormFn.apply(x, residual, weight, eps)
 
 
