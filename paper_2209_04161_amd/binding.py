@@ -822,6 +822,11 @@ def amsim_cache_attention(cache, page_table, lengths, q, starts, max_new, max_le
         out, o_tok, o_head = torch.empty(shape, dtype=dt, device=dev), q_heads * d, d
     else:
         o_tok, o_head = _check_heads(out, "out", dt, shape, dev)
+        if not out.is_contiguous() and total and q_heads:
+            # the shorter of the two strides first: each has to pass what lies below it
+            (a, n), (b, m) = sorted((s, c) for s, c in ((o_tok, total), (o_head, q_heads)))
+            if (n > 1 and a < d) or (m > 1 and b < (n - 1) * a + d):
+                raise ValueError("out must not overlap itself")
     if scale is None:
         scale = d ** -0.5
     max_new, max_len, window = int(max_new), int(max_len), int(window)
