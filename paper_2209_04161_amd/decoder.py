@@ -69,6 +69,8 @@ class DecoderBlock(torch.nn.Module):
 class Decoder(torch.nn.Module):
     def __init__(self, blocks, width, heads, kv_heads, hidden, lut, m_bits, head_dim=None):
         super().__init__()
+        if blocks < 1:
+            raise ValueError("a decoder has one block at least")
         self.blocks = torch.nn.ModuleList(
             [DecoderBlock(width, heads, kv_heads, hidden, lut, m_bits, head_dim) for _ in range(blocks)])
         self.norm = modules.RMSNorm(width, device=lut.device)
