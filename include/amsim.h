@@ -261,11 +261,14 @@ int approx_mul_ew_ex(const amsim_options *opt, int64_t n, const float *a, const 
  * multiplier is weighed against: 8-bit integers with FP32 scales.  They are exact operators: no
  * product of theirs goes through a table.
  *   - dtype: the element type of activations, AMSIM_F32, AMSIM_BF16 or AMSIM_F16.  All arithmetic is in
- *     FP32 (denormals read as zero) or in integers; a result is rounded once, to nearest even.
+ *     FP32 (denormals read as zero) or in integers, but for the two products of the attention, whose operands
+ *     are FP16; a result is rounded once, to nearest even.  There the cache's integers are exact; q is exact in
+ *     16-bit types and has 22 bits in FP32, the softmax's numerators have 11 bits for 16-bit types and 22 for
+ *     FP32, each but for 2^-38 of the row's largest; sums and maxima are FP32.
  *   - A quantised row or page stands for q * scale: scale = amax / 127 of its largest magnitude amax,
  *     q in [-127, 127] rounded to nearest even (of a row: of x times the FP32 number 127 * (1 / amax)).
  *     A row below 2^-100 has q = 0 and scale 0; one that holds an Inf or NaN has a NaN scale, so that
- *     everything computed from it is NaN.
+ *     everything computed from it is NaN (its integers then say nothing).
  *   - Row strides (ld*) are in elements, at least the row's length; rows need no alignment beyond their
  *     element's.  A workspace is 16-byte aligned (else AMSIM_ERR_INVALID_ARG).
  *   - Inputs may not overlap outputs except where said.
@@ -317,8 +320,9 @@ int amsim_gemm_i8(int64_t m, int64_t n, int64_t k, const int8_t *a, int64_t lda,
  * sequence's tokens [i * page_tokens, (i + 1) * page_tokens); lengths[b] counts its tokens including the new
  * ones; its new tokens, the last ones, are rows starts[b] .. starts[b + 1] - 1 of the call's tensors
  * (starts: batch + 1 numbers, rising; total_new rows in all).  On the host: max_new and max_len, bounds of
- * the new tokens and of the length of any sequence (a longer one is cut to them).  A page number
- * outside the cache is not written, and reads as NaN. */
+ * the new tokens and of the length of any sequence (a longer one is cut to them; result rows of no sequence's
+ * new tokens are not written).  A page number outside the cache is not written, and reads as NaN.  Entries past a
+ * sequence's length may be any number. */
 typedef struct amsim_cache8 {
     int8_t *k, *v;
     float *k_scale, *v_scale;
@@ -330,7 +334,11 @@ typedef struct amsim_cache8 {
  * head * k_head + i, and v likewise) and writes them to their pages.  A page's scale is that of the
  * largest magnitude written to it: where new tokens raise it, the integers of the page's earlier tokens
  * are rounded to the new scale, q = round(q * old / new).  The first token of a page starts its scale
- * anew.  No two sequences may share a page that gets new tokens. */
+ * anew.  No two sequences may share a page that gets new tokens.
+ *
+ * A page's scale is one for all of its tokens, later ones of the same call included: how a key or value is
+ * rounded, and with it a token's result, depends on what follows it in its page and on how a prompt is cut
+ * into calls.  Which keys a token sees does not. */
 int amsim_cache_append(const amsim_cache8 *cache, int64_t batch, const int32_t *page_table, int64_t ld_table,
                        const int32_t *lengths, const int32_t *starts, int64_t total_new, int64_t max_new, int dtype,
                        const void *k, int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,

@@ -336,13 +336,15 @@ __device__ __forceinline__ int tile_token(int t, int i)
 // the end; one workgroup for each chunk of the keys, whose sums combine_kernel joins where there are
 // several.  For few rows: each key and value is read once, by one wave, straight into the registers that
 // the matrix instructions take, and the kernel is bound by memory: 64 sequences of up to 8192 tokens, 8 key heads
-// of 128: 156 us, 4.5 TB/s; one of 131001: 61 us, 4.4 TB/s.
+// of 128: 156 us, 4.5 TB/s (FP32: 163); one of 131001: 62 us, 4.3 TB/s (FP32: 64).  Of 17 to 32 rows each 16 read the
+// cache: 16 sequences of 4096 tokens, 8 key heads of 128, 24 rows: 45 us, against 34 for 16 rows.
 //
 // S^T = K Q^T (tokens down, rows across), P = 2^(S - max), O^T = V^T P^T: S^T's registers are the operand that
 // the second product takes, and a row's maximum and sum stay in its lanes.  K and V go in as FP16 integers
 // (exact) and the scales are applied to S and to each tile's O.  q is scaled by a power of two to 2^15 and
 // P by 2^14, so that FP16 holds q exactly (FP32's: 22 bits, as the sum of two) and P to 11 bits (22)
-// down to 2^-28 of the row's largest.
+// down to 2^-28 of the row's largest.  (P in FP16 is what lets one matrix instruction take it; FP32 matrix
+// instructions have a sixteenth of the rate.)
 template <typename T, int DT, bool WHOLE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 4 && DT <= 128 ? 3 : 2) void attend_rows_kernel(AttnArgs a)
 {
@@ -604,10 +606,14 @@ __device__ __forceinline__ int k_place(int r, int c)
 // The same for many rows: 32 to a wave, 128 to a team of four waves, which turns each tile of 64 keys into FP16
 // once, in LDS (twice the tile: the next one is converted while the waves work on this one).  With two teams each takes
 // every other tile, for the same rows, and the first adds the second's sums to its own at the end.  Bound by the
-// matrix instructions and, next to them, by the exponentials: what a score costs is one maximum, one
-// multiply-add, one exponential, one addition and half a conversion.  Two prompts of 4096 tokens, 32 heads of 128 over 8
-// key heads, causal: 362 to 377 us, 0.7 PFLOP/s, 60% of what a large FP16 product reaches.  (The two waves of a SIMD in
-// turns, one multiplying while the other does the rest: 474 us; 256 rows to a workgroup: the same time.)
+// instructions that a wave issues in turn: of two prompts of 4096 tokens, 32 heads of 128 over 8 key heads, causal,
+// BF16 (377 to 392 us, 0.7 PFLOP/s), the matrix units take 29% of the cycles and vector instructions 45%.  Of those, some 370
+// for a wave and tile, about 100 turn bytes into FP16 for the next tile, the rest is the softmax: a maximum, a
+// multiply-add, an exponential, an addition and half a conversion for each score, and masks and O's rescaling where they are due.
+// (The two waves of a SIMD in turns, one multiplying while the other does the rest, and 256 rows to a workgroup were
+// slower and the same, against 412 and 378 us at those times.)  One prompt of 2048, 32 heads of 128 over 8, FP32: 122
+// us; 16 heads of 256 over 8: BF16 156, FP32 247 us, then 26 for the join.  Heads over 128, and over 64 in FP32, keep
+// some values in scratch memory.
 //
 // 32 x 32 tiles: S^T of 32 tokens and 32 rows leaves a lane 16 scores of one row, the rows of K in LDS in such an
 // order that they are two runs of 8 tokens, the operand of O^T = V^T P^T.  The scale of a page's values
@@ -1124,8 +1130,8 @@ AttnPlan plan_attention(const amsim_cache8 *c, int64_t batch, int64_t q_heads, i
     const int64_t seen = window > 0 && window + p.span < max_len ? window + p.span : max_len;
     const int64_t units = batch * c->heads * p.tiles;
     // splits so that some 2048 workgroups run, with 256 keys at least for each; of those with many rows (whose sums
-    // are more to join: 45 against 52 us for a chunk of 509 tokens over 1024 keys each) one for each compute unit, with
-    // 1024 keys, or for large heads (one team) two
+    // are more to join: 49 against 57 us for a chunk of 509 tokens over 1024 keys each, by one team) one for each compute
+    // unit, with 1024 keys, or for large heads (one team) two
     const int64_t least = p.span == 16 ? 256 : 1024;
     int64_t splits = units > 0 ? (p.span == 16 ? 2048 : c->head_dim <= 128 ? 256 : 512) / units : 1;
     const int64_t each = p.span == 16 ? ceil_div(seen, least) : seen / least;
@@ -1136,9 +1142,9 @@ AttnPlan plan_attention(const amsim_cache8 *c, int64_t batch, int64_t q_heads, i
     // workgroups, 18.9 against 25.0 for 256, 31.8 against 36.4 for 512; more of them fill the GPU with 4 waves each)
     p.wide = p.span == 16 && seen > 256 && seen * c->head_dim <= 1 << 17 && units <= 512;
     if (splits < 1 || p.wide) splits = 1;
-    // two teams of waves share a tile of rows' keys where that leaves no compute unit without a workgroup: a chunk of
-    // 509 tokens, window 1024, 12 heads of 64, 3 sequences: 37 against 45 us; 2048 tokens of 12 heads of 64: 40 against 53 us
-    // for two chunks of keys without
+    // two teams of waves share a tile of rows' keys where that leaves no compute unit without a workgroup (times with
+    // the append): a chunk of 509 tokens, window 1024, 12 heads of 64, 3 sequences: 40 against 49 us; 2048 tokens of
+    // 12 heads of 64: 50 against 62 us for two chunks of keys without
     if (p.span > 16) p.wide = c->head_dim <= 128 && seen > 64 && units * splits <= 256;
     p.chunk = int(ceil_div(ceil_div(seen, splits), 256) * 256);
     if (p.chunk < 256) p.chunk = 256;

@@ -125,9 +125,10 @@ __device__ __forceinline__ void wait_copies()
 // ALIGNED (rows at multiples of 16 bytes): through a ring of STAGES buffers in LDS; the operands of a half are read
 // into registers while the half before is multiplied, and the copies of the next STAGES - 1 steps are under
 // way.  Otherwise (and the last step, where it is not whole) through registers and two buffers.
-// Tiles of 256: 8192 x 8192 x 8192 484 us, 2.27 POP/s, 8192 x 8192 x 4096 276 us, 2.0 POP/s, bound by the matrix
-// instructions; of 128: 2048 x 2048 x 4096 29 us, 1.2 POP/s; of 64: 48 x 16384 x 4096 18 us, 3.6 TB/s of weights, bound
-// by memory, 1000 x 777 x 1111 12.5 us, bound by latency.
+// Tiles of 256: 8192 x 8192 x 8192 465 to 502 us, 2.2 to 2.4 POP/s, 8192 x 8192 x 4096 264 to 284 us, 1.9 to 2.1 POP/s,
+// as the library's product (the matrix units are busy 49% of the cycles); of 128: 2048 x 2048 x 4096 29 us, 1.2
+// POP/s, one workgroup of four waves to a compute unit; of 64: 48 x 16384 x 4096 19.5 us, 3.4 TB/s of weights, bound by memory
+// (13 us where the weights are in the last-level cache), 1000 x 777 x 1111 13 us, bound by latency.
 //
 // In LDS a row has 128 bytes, 8 pieces of 16, whose order is turned by the row's number: a 16-byte read of a wave is
 // served 16 lanes at a time, lanes 0-3, 12-15, 20-23 and 24-27 first, then 4-11, 16-19 and 28-31, and these lie in

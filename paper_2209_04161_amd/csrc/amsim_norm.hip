@@ -194,7 +194,7 @@ struct BwdArgs {
 // A row stays in registers between the sum and dx, and so do the owner's sums for dw over all of its rows.
 // 6000 x 2048 FP32 with dh: 37 us, 5.3 TB/s (192 MB).  (Reading the next row ahead takes registers from
 // waves that would hide the latency: 94 against 63 us for 8192 x 4096 BF16.)  Above 16384 elements some of a thread's
-// values go to scratch memory.
+// values go to scratch memory: 1024 x 32768 BF16 215 us, three times what 2048 x 16384 takes (74 us), FP32 255 us.
 template <typename T, int THREADS, int CH>
 __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void norm_bwd_kernel(BwdArgs a)
 {

@@ -75,7 +75,8 @@ __device__ __forceinline__ void store8(T *p, int64_t left, const float (&v)[8])
     }
 }
 
-// The integer of x at the reciprocal scale inv: rounded to nearest, ties to even.  A NaN gives 0.
+// The integer of x at the reciprocal scale inv: rounded to nearest, ties to even.  A NaN gives -127 (the scale beside
+// it is a NaN too).
 __device__ __forceinline__ int quantised(float x, float inv)
 {
     const float q = __builtin_rintf(x * inv);

@@ -176,7 +176,7 @@ def rms_norm(x, weight, eps=1e-6, residual=None):
 
 
 class RMSNorm(torch.nn.Module):
-    """y = h / rms(h) * weight over the last dimension, h = x + residual; exact FP32 arithmetic.
+    """y = h / rms(h) * weight over the rows of x [tokens, features], h = x + residual; FP32 arithmetic, an FP32 weight.
 
     forward(x) gives y; forward(x, residual) gives (y, h).  quantized() gives the same with y in 8 bits
     and a scale for each token, for an 8-bit product (no gradient)."""
