@@ -312,7 +312,7 @@ int amsim_gemm_i8(int64_t m, int64_t n, int64_t k, const int8_t *a, int64_t lda,
 
 /* A paged cache of keys and values in 8 bits, with one scale for each page (block of tokens) and head:
  * k [pages][heads][page_tokens][head_dim], v [pages][heads][head_dim][page_tokens] (a page's values are
- * held transposed), k_scale and v_scale [pages][heads].  Device memory of the caller, k and v 16-byte
+ * held transposed), k_scale and v_scale [pages][heads], not negative.  Device memory of the caller, k and v 16-byte
  * aligned; nothing in it has to be initialised.  page_tokens 32, 64, 128 or 256; head_dim a multiple of 16
  * up to 256; else AMSIM_ERR_UNSUPPORTED.
  *
